@@ -20,12 +20,13 @@ __device__ __forceinline__ void row_range(const int32_t *__restrict__ rank_off, 
 // A wavefront takes the choices part, part + parts, ... of a token: the token's k positions lie in its lanes, a ballot gives the choices whose row is
 // in range, and the token's gradient stays in registers (VPL 16-byte vectors a lane) while its rows pass; of rows wider than that it is read again for every
 // row (from the caches).  The sum over a row is each lane's in ascending order, then a tree over the lanes: the same in every run.
+// dy may be y: a row's vectors are all read ahead of the stores to them, an order that the compiler keeps because neither pointer is __restrict__.
 // Bound by HBM, each row read and written once: 16384 tokens, 8 choices, rows of 4 KB 216 us, 5.3 TB/s (a large copy reaches 4.9); 64 tokens 3.7 us.
 template <bool BF16, int VPL>
-__global__ __launch_bounds__(256) void combine_backward_kernel(const uint4 *__restrict__ dout, const uint4 *__restrict__ y,
+__global__ __launch_bounds__(256) void combine_backward_kernel(const uint4 *__restrict__ dout, const uint4 *y,
                                                                const int32_t *__restrict__ perm_pos, const float *__restrict__ weight, int64_t T,
                                                                int k, int row_vec, const int32_t *__restrict__ rank_off, int rank, int parts,
-                                                               uint4 *__restrict__ dy, float *__restrict__ dweight) {
+                                                               uint4 *dy, float *__restrict__ dweight) {
     constexpr int NV = BF16 ? 8 : 4;   // values per vector
     const int lane = (int)threadIdx.x & 63;
     const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -93,10 +94,11 @@ __global__ __launch_bounds__(256) void combine_backward_kernel(const uint4 *__re
 // A wavefront takes 64 vectors of a token's row (consecutive wavefronts consecutive parts of it); positions and ballot as above, two
 // rows in flight (16384 tokens, one choice 25.3 us, 29.2 with four in flight; 8 choices the same).  A surplus load has a descriptor without records,
 // reads nothing and gives zeros.  Bound by HBM: 16384 tokens, 8 choices, rows of 4 KB 104 us, 5.8 TB/s; 64 tokens 3.6 us.
+// dx may be dx_shared, so neither is __restrict__.
 template <bool BF16>
 __global__ __launch_bounds__(256) void permute_backward_kernel(const char *__restrict__ dxp, const int32_t *__restrict__ perm_pos, int64_t T, int k,
                                                                int row_vec, int pieces, const int32_t *__restrict__ rank_off, int rank,
-                                                               const uint4 *__restrict__ dx_shared, uint4 *__restrict__ dx) {
+                                                               const uint4 *dx_shared, uint4 *dx) {
     constexpr int NV = BF16 ? 8 : 4, BATCH = 2;
     const int lane = (int)threadIdx.x & 63;
     const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
