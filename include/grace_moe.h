@@ -472,8 +472,10 @@ size_t grace_ffn_backward_workspace_bytes(int32_t rows, int32_t d, int32_t f, in
  *     out_i = scale * grad_i,   scale = 1 if norm <= max_norm, else max_norm / norm
  * (a norm that is NaN makes everything NaN, an infinite one zeros and NaN).  Squares are summed in 64 bits in an order that only the sizes
  * decide.  grace_clip_grad_norm is the two calls with fewer launches; they are apart for a norm that other ranks' gradients are part of.
- * HOST: grads, out [n] device pointers, aligned to their elements, out[i] either grads[i] (in place) or apart from all gradients; numel
- * [n], at least 0; dtypes [n] (grace_dtype).  DEVICE: norm fp32, one value; ws of grace_grad_norm_workspace_bytes(n) bytes, 8-byte aligned.
+ * HOST: grads, out [n] device pointers, aligned to their elements; numel [n], at least 0; dtypes [n] (grace_dtype).  An out[i] is
+ * grads[i] (in place) or apart from it, and apart from every other gradient and output: a gradient that is in the list twice (of a weight that two layers
+ * share) is refused in place; with outputs of their own gradients may overlap.  Each entry of the list counts towards the norm.
+ * DEVICE: norm fp32, one value; ws of grace_grad_norm_workspace_bytes(n) bytes, 8-byte aligned; both apart from all else.
  * max_norm is finite and not negative. */
 int grace_grad_norm(const void *const *grads, const int64_t *numel, const int32_t *dtypes, int32_t n, float *norm, void *ws, void *stream);
 int grace_clip_grads(const void *const *grads, const int64_t *numel, const int32_t *dtypes, int32_t n, const float *norm, float max_norm,

@@ -896,7 +896,8 @@ def grace_grad_norm(grads: Sequence[torch.Tensor], norm: Optional[torch.Tensor] 
 
 
 def grace_clip_grads(grads: Sequence[torch.Tensor], norm: torch.Tensor, max_norm: float, out: Optional[Sequence[torch.Tensor]] = None):
-    """The gradients scaled by min(1, max_norm / norm), in place or into `out` -> the scaled tensors; see grace_moe.h."""
+    """The gradients scaled by min(1, max_norm / norm), in place or into `out` -> the scaled tensors.  In place no two of them may overlap, into
+    `out` no output anything else; see grace_moe.h."""
     src, numel, dtypes, n, dst = _gradients(grads, out)
     _need(norm, "norm", torch.float32, 1)
     _check(load_library().grace_clip_grads(src, numel, dtypes, n, _dp(norm), max_norm, dst, _stream()))
@@ -905,7 +906,7 @@ def grace_clip_grads(grads: Sequence[torch.Tensor], norm: torch.Tensor, max_norm
 
 def grace_clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None,
                          norm: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """grace_grad_norm and grace_clip_grads by that norm, with fewer launches -> the norm before clipping; see grace_moe.h."""
+    """grace_grad_norm and grace_clip_grads by that norm, with fewer launches -> the norm before clipping; the tensors as in grace_clip_grads."""
     native = _native()
     if native:
         return _made(native.clip_grad_norm(grads, max_norm, out, norm, ws, _stream_of(grads[0] if len(grads) else None)))

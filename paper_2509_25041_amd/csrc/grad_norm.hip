@@ -6,6 +6,8 @@
 // the norm is the same in every run.  The tensors' addresses travel as kernel arguments: nothing is copied to the device, and a captured
 // launch keeps them.
 #include <cmath>
+#include <memory>
+#include <new>
 
 #include "bf16.h"
 #include "common.h"
@@ -199,8 +201,30 @@ static int check(const char *who, const void *const *grads, const int64_t *numel
     return GRACE_OK;
 }
 
+// Memory of a call: what is written has to be apart from everything else, or workgroups would read and scale the same values in any order.
+struct Range {
+    uintptr_t begin, end;
+    int32_t index;             // of the gradient or output, -1: norm or workspace
+    bool written;
+};
+
+// No written range may meet another.  In order of their beginnings a range meets one ahead of it where the latter's end is past its beginning.
+static int check_apart(const char *who, Range *r, size_t n) {
+    std::sort(r, r + n, [](const Range &a, const Range &b) { return a.begin < b.begin; });
+    uintptr_t any_end = 0, written_end = 0;
+    for (size_t i = 0; i < n; ++i) {
+        if (r[i].begin < (r[i].written ? any_end : written_end))
+            return r[i].index < 0 ? fail(GRACE_EINVAL, "%s: norm or workspace overlaps a gradient or output", who)
+                                  : fail(GRACE_EINVAL, "%s: %s %d overlaps other memory of the call", who, r[i].written ? "output" : "gradient", r[i].index);
+        any_end = std::max(any_end, r[i].end);
+        if (r[i].written) written_end = std::max(written_end, r[i].end);
+    }
+    return GRACE_OK;
+}
+
+// ws: null where the call has none and reads the norm, else the norm is written.
 static int check_outputs(const char *who, const void *const *grads, const int64_t *numel, const int32_t *dtypes, int32_t n, void *const *out,
-                         float max_norm) {
+                         float max_norm, const float *norm, const void *ws) {
     if (!(max_norm >= 0.0f) || std::isinf(max_norm)) return fail(GRACE_EINVAL, "%s: max_norm=%g invalid", who, (double)max_norm);
     if (n > 0 && !out) return fail(GRACE_EINVAL, "%s: null host pointer", who);
     for (int i = 0; i < n; ++i) {
@@ -210,7 +234,21 @@ static int check_outputs(const char *who, const void *const *grads, const int64_
         if (b % el) return fail(GRACE_EINVAL, "%s: output %d is not aligned to its elements", who, i);
         if (a != b && a < b + bytes && b < a + bytes) return fail(GRACE_EINVAL, "%s: output %d overlaps its gradient in part", who, i);
     }
-    return GRACE_OK;
+    Range few[2 * FEW_TENSORS + 2];
+    std::unique_ptr<Range[]> many;
+    if (n > FEW_TENSORS) many.reset(new (std::nothrow) Range[2 * (size_t)n + 2]);
+    Range *const r = n > FEW_TENSORS ? many.get() : few;
+    if (!r) return fail(GRACE_ENOMEM, "%s: no host memory for %d gradients", who, n);
+    size_t count = 0;
+    for (int i = 0; i < n; ++i) {
+        if (numel[i] == 0) continue;
+        const uintptr_t a = (uintptr_t)grads[i], b = (uintptr_t)out[i], bytes = (uintptr_t)numel[i] * (dtypes[i] == GRACE_F32 ? 4 : 2);
+        r[count++] = Range{b, b + bytes, i, true};
+        if (a != b) r[count++] = Range{a, a + bytes, i, false};
+    }
+    r[count++] = Range{(uintptr_t)norm, (uintptr_t)norm + sizeof(float), -1, ws != nullptr};
+    if (ws) r[count++] = Range{(uintptr_t)ws, (uintptr_t)ws + grace_grad_norm_workspace_bytes(n), -1, true};
+    return check_apart(who, r, count);
 }
 
 template <typename F>
@@ -291,9 +329,10 @@ extern "C" int grace_grad_norm(const void *const *grads, const int64_t *numel, c
 extern "C" int grace_clip_grads(const void *const *grads, const int64_t *numel, const int32_t *dtypes, int32_t n, const float *norm_in,
                                 float max_norm, void *const *out, void *stream) {
     int rc = norm::check("clip_grads", grads, numel, dtypes, n);
-    if (rc == GRACE_OK) rc = norm::check_outputs("clip_grads", grads, numel, dtypes, n, out, max_norm);
     if (rc != GRACE_OK) return rc;
     if (!norm_in || ((uintptr_t)norm_in & 3)) return fail(GRACE_EINVAL, "clip_grads: null or unaligned device pointer");
+    rc = norm::check_outputs("clip_grads", grads, numel, dtypes, n, out, max_norm, norm_in, nullptr);
+    if (rc != GRACE_OK) return rc;
     const int chunk = norm::chunk_elements(numel, n);
     if (chunk == 0) return fail(GRACE_ESHAPE, "clip_grads: too many elements");
     return norm::for_launches(grads, out, numel, dtypes, n, chunk, [&](const auto &a, int) {
@@ -307,10 +346,11 @@ extern "C" int grace_clip_grads(const void *const *grads, const int64_t *numel, 
 extern "C" int grace_clip_grad_norm(const void *const *grads, const int64_t *numel, const int32_t *dtypes, int32_t n, float max_norm,
                                     void *const *out, float *norm_out, void *ws, void *stream) {
     int rc = norm::check("clip_grad_norm", grads, numel, dtypes, n);
-    if (rc == GRACE_OK) rc = norm::check_outputs("clip_grad_norm", grads, numel, dtypes, n, out, max_norm);
     if (rc != GRACE_OK) return rc;
     if (!norm_out || !ws || ((uintptr_t)ws & 7) || ((uintptr_t)norm_out & 3))
         return fail(GRACE_EINVAL, "clip_grad_norm: null or unaligned device pointer");
+    rc = norm::check_outputs("clip_grad_norm", grads, numel, dtypes, n, out, max_norm, norm_out, ws);
+    if (rc != GRACE_OK) return rc;
     const int chunk = norm::chunk_elements(numel, n);
     if (chunk == 0) return fail(GRACE_ESHAPE, "clip_grad_norm: too many elements");
     hipStream_t st = (hipStream_t)stream;
