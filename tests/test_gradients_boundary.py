@@ -134,3 +134,13 @@ def test_ffn_backward_assembly_keeps_its_wait_states():
     n, found = asm_hazards.check("ffn_backward.hip")
     assert n > 30
     assert found == [], "\n".join(found)
+
+
+def test_rows_backward_refuses_more_wavefronts_than_a_launch_takes(lib):
+    """T * k fits its range and a row its own, the launch's work-items do not: the entry of T = 1 << 28 above, whose statuses are not looked at there."""
+    T, d = 1 << 28, 4096
+    for k in (1, 2, 7):
+        for dt in (F32, BF16):
+            assert lib.grace_permute_backward(AT, AT, T, k, d, dt, None, 0, None, AT, None) == ESHAPE
+            assert lib.grace_combine_backward(AT, AT, AT, AT, T, k, d, dt, None, 0, AT, AT, None) == ESHAPE
+            assert "too many rows" in grace.grace_last_error()
