@@ -419,7 +419,14 @@ int grace_combine_share(const void *y, const int32_t *perm_pos, const float *top
  *
  * Rank share: with rank_off [R+1] (from grace_permute) and rank a call is about the rows [rank_off[rank], rank_off[rank+1]) alone;
  * rank_off == NULL: about all T*k rows (rank is then not used).  An assignment whose row is not among them, or whose perm_pos is not
- * in [0, T*k), adds nothing and its row is not touched. */
+ * in [0, T*k), adds nothing and its row is not touched.
+ *
+ * Several ranks: what a call gives for a rank is that rank's part.  dtopk_weight and dx are to be summed over the ranks that a token's rows are
+ * on (dx_shared added once).  The weights' gradients are of instances: those of an expert's instances are to be summed over the ranks that
+ * host it ahead of the optimizer, or its replicas no longer hold the same weights, and ahead of the global norm, which counts every expert
+ * once: the squares of the parts do not add up to the square of their sum.
+ *
+ * No output overlaps an input, another output or a workspace unless a call says so. */
 
 /* Gradient of grace_combine (Section 1's aggregation) for the rows and the gate weights:
  *     dy[perm_pos[t*k+j]] = topk_weight[t,j] * dout[t],   dtopk_weight[t,j] = sum_c dout[t,c] * y[perm_pos[t*k+j],c]

@@ -888,7 +888,8 @@ def _norm_and_ws(grads, norm, ws):
 
 
 def grace_grad_norm(grads: Sequence[torch.Tensor], norm: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Global 2-norm of the gradients (fp32 and bf16, any lengths), as one fp32 value on the device; see grace_moe.h."""
+    """Global 2-norm of the gradients (fp32 and bf16, any lengths), as one fp32 value on the device; see grace_moe.h.  Of several ranks' gradients:
+    the root of the ranks' summed squares, each expert counted once, with the sum of its instances' gradients."""
     src, numel, dtypes, n, _ = _gradients(grads)
     norm, ws = _norm_and_ws(grads, norm, ws)
     _check(load_library().grace_grad_norm(src, numel, dtypes, n, _dp(norm), _dp(ws), _stream()))

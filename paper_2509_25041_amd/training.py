@@ -15,7 +15,10 @@ class GraceMoEBackward:
 
     `backward` follows a `forward` of the layer (eager or replayed) and uses what that step left in the layer's buffers: the
     dispatch order, the dispatched rows, the experts' results and the gate weights; the experts' hidden activations are computed again.
-    On a rank that does not host every instance the gradients are those of the rank's own rows, as the layer's output is.
+    On a rank that does not host every instance the gradients are those of the rank's own rows, as the layer's output is: `dx` and `dlogits`
+    are to be summed over the ranks (the shared experts' part of `dx` is in every rank's).  `dw` is of the rank's instances: an expert that is on
+    several ranks has the sum of its instances' gradients, which has to be made (an all-reduce among the ranks that host it) before
+    grace_grad_norm, grace_clip_grads and the optimizer; otherwise its replicas drift apart, and the norm of the parts is not that of their sum.
 
     Results are in buffers of this object, overwritten by the next step: `dx` [T,d] (through the experts and the shared experts),
     `dlogits` [T,E] (the gate's own weights are the caller's), and the weights' gradients `dw` (gate, up, down [S,...]) and `dshared`
@@ -41,7 +44,7 @@ class GraceMoEBackward:
         self.ws = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
 
     def gradients(self) -> List[torch.Tensor]:
-        """The weights' gradients, for grace_clip_grad_norm and the optimizer."""
+        """The weights' gradients, for grace_clip_grad_norm and the optimizer (where experts are replicated, after their instances' sums)."""
         return list(self.dw) + list(self.dshared or ())
 
     def backward(self, dout: torch.Tensor, logits: torch.Tensor, x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
