@@ -477,7 +477,8 @@ size_t grace_ffn_backward_workspace_bytes(int32_t rows, int32_t d, int32_t f, in
 
 /* Global 2-norm of n gradients, norm = sqrt(sum of the squares of all their elements), and their clipping by it:
  *     out_i = scale * grad_i,   scale = 1 if norm <= max_norm, else max_norm / norm
- * (a norm that is NaN makes everything NaN, an infinite one zeros and NaN).  Squares are summed in 64 bits in an order that only the sizes
+ * (norm and scale are fp32 values; a norm that is NaN makes everything NaN, an infinite one, also of finite gradients whose norm is past
+ * the range of fp32, zeros and NaN).  Squares are summed in 64 bits in an order that only the sizes
  * decide.  grace_clip_grad_norm is the two calls with fewer launches; they are apart for a norm that other ranks' gradients are part of.
  * HOST: grads, out [n] device pointers, aligned to their elements; numel [n], at least 0; dtypes [n] (grace_dtype).  An out[i] is
  * grads[i] (in place) or apart from it, and apart from every other gradient and output: a gradient that is in the list twice (of a weight that two layers

@@ -739,7 +739,8 @@ def grace_combine_backward(dout: torch.Tensor, y: torch.Tensor, perm_pos: torch.
                            rank_off: Optional[torch.Tensor] = None, rank: int = 0, dy: Optional[torch.Tensor] = None,
                            dtopk_weight: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Gradient of grace_combine -> (dy [T*k,d], dtopk_weight [T,k]), of all rows or, with rank_off, of those of `rank` (others are not
-    touched; a fresh dy starts as zeros); see grace_moe.h."""
+    touched; a fresh dy then starts as zeros).  Without rank_off a fresh dy holds anything in rows that no assignment's perm_pos names; see
+    grace_moe.h."""
     native = _native()
     if native:
         return _made(native.combine_backward(dout, y, perm_pos, topk_weight, rank_off, rank, dy, dtopk_weight, _stream_of(y)))

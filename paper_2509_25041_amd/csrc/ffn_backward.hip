@@ -35,9 +35,20 @@ using SMALL = Shape<64, 64, 64, 4, 4, 4, 1>;
 enum class Tiles { LARGE, LOWER, MEDIUM, SMALL };
 
 // dh and gates: time of a launch by its rounds of tiles.  Measured for sums of 2048 (32 steps), us a round: LARGE 62, LOWER 52; MEDIUM 47 with two workgroups on
-// every compute unit, 30 with one; SMALL 24 and 17.  (16 experts, d = 2048, f = 1024, us with LARGE, MEDIUM, SMALL: dh of 128 rows 46, 25, 18, of 2048 49, 28,
-// 33, of 8192 60, 66, -; gates of 128 rows 60, 54, 43, of 2048 67, 59, 64, of 8192 135, 118, -.  Whole pass with LARGE and LOWER, us: dh of 8192 rows
-// 363, 353, of 8001 rows of two shared experts, f = 1408 698, 684, of 4096 of 2 experts, d = 4096, f = 14336 3201, 3207; gates 363, 347, 699, 696, 3206, 3202.)
+// every compute unit, 30 with one; SMALL 24 and 17.  Only the ratios matter, and they are taken to be the same for other widths d; where d is so small that
+// a tile is mostly start and epilogue that was not measured.  Whole pass, us, with these tiles for one launch and the rules' for the other two, and
+// which are chosen; 16 experts, d = 2048, f = 1024 unless said:
+//                                             dh LARGE  LOWER MEDIUM SMALL          gates LARGE  LOWER MEDIUM SMALL
+//     16 rows of 8, d = 1024, f = 512            33.0   30.5   28.7   24.4  S              32.9   31.2   28.9   24.4  S
+//     128 rows                                    108    104    102     94  S               101     98     95     94  S
+//     512                                         123    124    115    113  S               114    115    107    113  S
+//     2048                                        164    154    146    149  M               152    144    145    153  M
+//     4096                                        205    191    191    200  M               197    190    202    222  LOWER
+//     8192                                        337    322    338    361  LOWER           338    321    331    382  LOWER
+//     16000 of 4, d = 1024, f = 512               162    157    156    172  M               155    167    162    191  L
+//     4096 of 2, d = 4096, f = 14336             3223   3215   3287   3688  L              3224   3204   3339   4111  L
+//     2000 of two shared, d = 1024, f = 1408      124    119    116    123  M               118    116    120    136  LOWER
+//     8001 of two shared, f = 1408                656    647    662    718  LOWER           654    660    667    791  L
 static double rounds_cost(Tiles shape, int64_t tiles, int n_cu) {
     if (shape == Tiles::LARGE || shape == Tiles::LOWER) return (shape == Tiles::LARGE ? 62.0 : 52.0) * (double)ceil_div(tiles, n_cu);
     const double both = shape == Tiles::MEDIUM ? 47.0 : 24.0, one = shape == Tiles::MEDIUM ? 30.0 : 17.0;
@@ -46,12 +57,21 @@ static double rounds_cost(Tiles shape, int64_t tiles, int n_cu) {
 }
 
 // dx and the weights' gradients, in one launch: time by the steps (64 positions of a sum) of its tiles; storing a weights' tile takes two steps' time.
-// SMALL tiles are for dx only, beside MEDIUM ones for the weights, and LARGE ones for the weights only, beside LOWER ones for dx (whole pass with LARGE ones for
-// both and so, us: two shared experts, 8001 rows, f = 1408 699, 652; 2000 rows 155, 131; 8192 rows of 16 experts 363, 362; 4096 rows of 2 experts, f = 14336
-// 3203, 3195).  Fitted to 16 measured sizes.  Whole pass with LARGE, MEDIUM, SMALL, us, and which one this chooses: 16 rows of 8 experts, d = 1024, f = 512
-// 31.2, 28.0, 24.4, S; 100 rows of 4, d = 512, f = 2048 56.5, 53.1, 35.2, S; 128 rows of 16, d = 2048, f = 1024 115, 111, 114, M; 2048 rows 167, 172, 186, L;
-// 8192 rows 344, 368, 431, L; 16000 rows of 4, d = 1024, f = 512 223, 175, 203, M; 4096 rows of 2, d = 4096, f = 14336 3356, 3946, 5170, L; two shared experts,
-// f = 1408, 2000 rows, d = 1024 135, 118, 137, M; 8001 rows, d = 2048 674, 765, 884, L.
+// SMALL tiles are for dx only, beside MEDIUM ones for the weights, and LARGE ones for the weights only, beside LOWER ones for dx; the fit is older than that and
+// still counts dx's tiles as 256 x 256 then.  Fitted to 16 measured sizes.  Whole pass, us, with LARGE tiles for both, LOWER and LARGE, MEDIUM for both, SMALL and
+// MEDIUM, the other launches by their rule, and which of the last three is chosen (LARGE: the first
+// of them); 16 experts, d = 2048, f = 1024 unless said:
+//     16 rows of 8, d = 1024, f = 512            33.0   30.9   28.0   24.5  SMALL
+//     100 rows of 4, d = 512, f = 2048           62.1   56.4   53.0   35.3  SMALL
+//     128 rows                                     99     98     94     96  MEDIUM
+//     512                                         115    116    113    115  MEDIUM
+//     2048                                        144    147    144    156  LARGE
+//     4096                                        194    190    202    233  LARGE
+//     8192                                        325    320    342    409  LARGE
+//     16000 of 4, d = 1024, f = 512               193    194    158    188  MEDIUM
+//     4096 of 2, d = 4096, f = 14336             3245   3223   3811   5096  LARGE
+//     2000 of two shared, d = 1024, f = 1408      158    134    118    137  MEDIUM
+//     8001 of two shared, f = 1408                687    652    753    852  LARGE
 static double joined_cost(Tiles shape, const FfnGrad &g, int n_cu) {
     struct Fit { int side, at_once; double start, step, step_full, tail; };   // us: of a launch, a step alone, a step on every unit, the last tiles' steps
     constexpr Fit large{256, 1, 5.0, 1.0, 1.9, 0.5}, medium{128, 2, 3.0, 0.65, 1.2, 0.25}, small{64, 2, 5.0, 0.3, 0.55, 0.0};
@@ -59,7 +79,7 @@ static double joined_cost(Tiles shape, const FfnGrad &g, int n_cu) {
     const double in_slots = (double)n_cu * fi.at_once, w_slots = (double)n_cu * fw.at_once;
     const double in = (double)expected_tiles<INPUT>(g, fi.side, fi.side), w = (double)expected_tiles<WEIGHTS>(g, fw.side, fw.side);
     const double in_steps = (double)steps_of<INPUT>(g), w_steps = (double)steps_of<WEIGHTS>(g);
-    const double longest = g.seg_off ? 1.75 * w_steps : w_steps;   // (experts with more rows than the mean)
+    const double longest = g.seg_off ? 1.75 * w_steps : w_steps;   // (experts with more rows than the mean: an assumption about skew, not a measurement)
     return fi.start + std::max({fi.step * in_steps, fw.step * longest, fi.step_full * in * in_steps / in_slots + fw.step_full * w * (w_steps + 2.0) / w_slots}) +
            fi.tail * std::min(w_steps, w_steps * w / w_slots);
 }

@@ -167,7 +167,7 @@ __global__ __launch_bounds__(THREADS) void clip_kernel(const Tensors<MOST> a, co
     if (!norm && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = v;
     const float scale = v <= max_norm ? 1.0f : max_norm / v;   // (a norm that is NaN scales by NaN)
     // from the last chunk to the first: the ones read last for the norm are in the caches still (403 M elements in 20 tensors, both kernels 473 ->
-    // 457 us, 438 with stores that bypass the caches; the bytes at the rate of a large copy 491)
+    // 457 us, 438 with stores that bypass the caches; the bytes at the rate of a large copy 480)
     for (int b = (int)blockIdx.x; b < a.chunks; b += (int)gridDim.x) {
         const int c = a.chunks - 1 - b;
         const Tensor t = a.t[tensor_of(a, c)];

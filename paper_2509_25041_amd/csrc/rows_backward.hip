@@ -21,7 +21,7 @@ __device__ __forceinline__ void row_range(const int32_t *__restrict__ rank_off, 
 // in range, and the token's gradient stays in registers (VPL 16-byte vectors a lane) while its rows pass; of rows wider than that it is read again for every
 // row (from the caches).  The sum over a row is each lane's in ascending order, then a tree over the lanes: the same in every run.
 // dy may be y: a row's vectors are all read ahead of the stores to them, an order that the compiler keeps because neither pointer is __restrict__.
-// Bound by HBM, each row read and written once: 16384 tokens, 8 choices, rows of 4 KB 216 us, 5.3 TB/s (a large copy reaches 4.9); 64 tokens 3.7 us.
+// Bound by HBM, each row read and written once: 16384 tokens, 8 choices, rows of 4 KB 216 us, 5.3 TB/s (a large copy reaches 5.0); 64 tokens 3.7 us.
 template <bool BF16, int VPL>
 __global__ __launch_bounds__(256) void combine_backward_kernel(const uint4 *__restrict__ dout, const uint4 *y,
                                                                const int32_t *__restrict__ perm_pos, const float *__restrict__ weight, int64_t T,
