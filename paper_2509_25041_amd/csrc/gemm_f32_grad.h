@@ -1,8 +1,8 @@
 // fp32 kernel of the FFN's backward products (ffn_grad.h) on v_mfma_f32_16x16x4_f32: products and sums in 32 bits.  64 x 64 tiles, sums in
 // steps of 32, four wavefronts (2 x 2) of 32 x 32 results.  Both operands lie in LDS as [32 positions of the sum axis][64], whichever way they
 // lie in memory; the next AHEAD steps' values are loaded to registers meanwhile.
-// Bound by the matrix cores and how well tiles fill: 4000 rows of 4 experts, d = 2048, f = 1408 1490 us, 124 of the 147 TFLOP/s that a large product
-// reaches; 1000 rows of 8, d = 1024, f = 2816 488 us, 94 (tiles of 64 of their rows hold 78 % of what they could).  Figures below: the latter's whole pass.
+// Bound by the matrix cores and how well tiles fill: 4000 rows of 4 experts, d = 2048, f = 1408 1505 us, 122 of the 147 TFLOP/s that a large product
+// reaches; 1000 rows of 8, d = 1024, f = 2816 487 us, 95 (tiles of 64 of their rows hold 78 % of what they could).  Figures below: the latter's whole pass.
 #pragma once
 #include <type_traits>
 
@@ -92,6 +92,12 @@ static_assert(THREADS / (BK / 4) == TILE / 2, "a thread's first vector is of the
 
 constexpr int F = TILE / 32;   // fragments of a wavefront along each side
 
+// A sum is made of parts of PART steps (256 terms), which are added up: a running sum of 8192 terms was off by 1.6e-6 of its norm, this is by 3.8e-7.  A part is
+// added while the next step's values are on their way to LDS (4000 rows of 4 experts, d = 2048, f = 1408 1495 -> 1520 us, behind the step's products 1533,
+// with the sums in LDS 1550).
+constexpr int PART = 8;
+static_assert(PART % AHEAD == 0, "a part begins with a round of steps");
+
 // One step's products.
 template <Product P>
 __device__ __forceinline__ void products(const Staged &sa, const Staged &sb, int wm, int wn, int lane, f32x4_t (&acc)[F][F]) {
@@ -138,20 +144,31 @@ __device__ __forceinline__ void tile(const FfnGrad &g, int block, Staged &sa, St
         a.template load<P == INPUT>(va[slot]);
         b.template load<P == INPUT>(vb[slot]);
     };
-    f32x4_t acc[F][F];
+    f32x4_t acc[F][F], sum[F][F];   // of the part, of the parts before it
 #pragma unroll
     for (int i = 0; i < F; ++i)
 #pragma unroll
-        for (int j = 0; j < F; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < F; ++j) acc[i][j] = sum[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    auto end_part = [&] {
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j) {
+                sum[i][j] += acc[i][j];
+                acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+    };
 #pragma unroll
     for (int s = 0; s < AHEAD; ++s) load(s);
     // A wavefront whose rows or columns are not there stages and keeps step, and leaves the matrix cores to the others (504 -> 493 us).
     const bool idle = wm * (TILE / 2) >= t.m || (P == GATES ? wn * (TILE / 4) : wn * (TILE / 2)) >= t.n;   // uniform
     auto all_steps = [&](auto works) {
         // (two buffers and one barrier a step took the same time)
-        auto step = [&](int slot) {
+        auto step = [&](int slot, bool begins_part) {
             A::store(sa, va[slot], tid);
             B::store(sb, vb[slot], tid);
+            if constexpr (works.value)
+                if (begins_part) end_part();   // (the first one: of zeros)
             __syncthreads();
             load(slot);
             if constexpr (works.value) products<P>(sa, sb, wm, wn, lane, acc);
@@ -160,16 +177,17 @@ __device__ __forceinline__ void tile(const FfnGrad &g, int block, Staged &sa, St
         int s = 0;
         for (; s + AHEAD <= steps; s += AHEAD) {
 #pragma unroll
-            for (int q = 0; q < AHEAD; ++q) step(q);   // (a register array is indexed by constants)
+            for (int q = 0; q < AHEAD; ++q) step(q, q == 0 && s % PART == 0);   // (a register array is indexed by constants)
         }
 #pragma unroll
         for (int q = 0; q < AHEAD - 1; ++q)
-            if (s + q < steps) step(q);
+            if (s + q < steps) step(q, false);
+        end_part();
     };
     if (idle) all_steps(std::false_type{});
     else all_steps(std::true_type{});
 
-    // value v of acc[i][j]: row 16 i + lane % 16, column 16 j + 4 (lane / 16) + v
+    // value v of sum[i][j]: row 16 i + lane % 16, column 16 j + 4 (lane / 16) + v
 #pragma unroll
     for (int i = 0; i < F; ++i) {
         const int row = wm * (TILE / 2) + i * 16 + (lane & 15);
@@ -186,7 +204,7 @@ __device__ __forceinline__ void tile(const FfnGrad &g, int block, Staged &sa, St
                 for (int v = 0; v < 4; ++v) {
                     if (!VEC) dh[v] = col + v < t.n ? to[0][v] : 0.0f;
                     float h, dg, du;
-                    swiglu_grad<false>(acc[i][j][v], acc[i][j + F / 2][v], dh[v], h, dg, du);
+                    swiglu_grad<false>(sum[i][j][v], sum[i][j + F / 2][v], dh[v], h, dg, du);
                     out[0][v] = h; out[1][v] = dg; out[2][v] = du;
                 }
 #pragma unroll
@@ -202,11 +220,11 @@ __device__ __forceinline__ void tile(const FfnGrad &g, int block, Staged &sa, St
             } else {
                 float *to = t.out + (int64_t)row * t.ldo + col;
                 if (VEC) {
-                    if (col < t.n) *(f32x4_t *)to = acc[i][j];
+                    if (col < t.n) *(f32x4_t *)to = sum[i][j];
                 } else {
 #pragma unroll
                     for (int v = 0; v < 4; ++v)
-                        if (col + v < t.n) to[v] = acc[i][j][v];
+                        if (col + v < t.n) to[v] = sum[i][j][v];
                 }
             }
         }
